@@ -693,8 +693,10 @@ int pod_paged_compact(pod_paged *cache, void *stream);
 /*
  * How a packed batch is walked: sequence e of the batch has the rows cu_rows[e] .. cu_rows[e + 1] - 1 (dev int32 [n + 1], from 0,
  * not decreasing, ending at total_rows) of the call's tensors, which are the last tokens its slot holds: call pod_paged_extend first.
- * Made once per batch and used for every layer: pod_paged_store, pod_paged_prefill.  plan: dev buffer of
- * pod_paged_plan_bytes(cfg, n, total_rows) bytes, 256-byte aligned.  Empty sequences are allowed.  Rows out of order, more rows
+ * Made once per batch and used for every layer: pod_paged_store, pod_paged_prefill; it serves until one of its slots is extended or freed.
+ * plan: dev buffer of pod_paged_plan_bytes(cfg, n, total_rows) bytes, 256-byte aligned.  Empty sequences are allowed.  The rows may have come
+ * by several calls of pod_paged_extend, and older tokens may be among them, as long as the first row's window still has all its window pages: each
+ * extend gives back those that its own first token no longer needs.  Rows whose window pages are gone, rows out of order, more rows
  * than a slot holds tokens, a slot outside the cache or named twice: the plan is empty (flag), and calls with it do nothing.
  */
 int pod_paged_plan_bytes(const pod_paged_config *cfg, int n, int total_rows, size_t *bytes);

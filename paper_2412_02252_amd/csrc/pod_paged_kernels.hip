@@ -420,6 +420,12 @@ __global__ __launch_bounds__(kBook) void paged_plan_kernel(pod_paged_view c, con
             len = c.lens[slot];
             bad = mark(seen, slot) || len < hi - lo || len > c.maxctx;
         }
+        if (c.nw && !bad && hi > lo) {
+            // What the rows attend by their own layers' keys starts at the first row's window (sink pages never go back).  Pages go back oldest
+            // first, so the rest is there if that window's first page behind the sink is.
+            const int first = len - (hi - lo), page = max((c.S + c.ps - 1) / c.ps, max(first - c.W + 1, 0) / c.ps);
+            bad = (int64_t)page * c.ps < len && c.wtable[(size_t)slot * c.width + page] < 0;
+        }
     }
     const bool refused = __syncthreads_or(bad) || n == 0;
     if (e == 0) {

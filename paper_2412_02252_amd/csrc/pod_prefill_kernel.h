@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256 * KS, 2) void prefill_kernel(typename params_of
     const unsigned k_dst0 = (unsigned)(uintptr_t)(lbyte_ptr)lds + grp * (2 * KBUF + 2 * VBUF) + wave * (16 * D * 2); // this wave's part of K slot 0
     const unsigned v_dst0 = k_dst0 + 2 * KBUF;                                                                        // ... of V slot 0
     // PAGED: a wave's 16 rows of a tile lie in one page (rows past the last token: in the last token's).  A page that is gone holds window
-    // keys that every row masks; any page serves.
+    // keys that every row masks (the plan refuses rows that would not); any page serves.
     [[maybe_unused]] int ps_shift = 0;
     if constexpr (PAGED) ps_shift = 31 - __builtin_clz((unsigned)p.c.ps);
     auto page_at = [&](int kt) __attribute__((always_inline)) { return min(kt * kBN + 16 * wave, n - 1); }; // the wave's first row of tile kt
