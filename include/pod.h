@@ -669,7 +669,8 @@ int pod_paged_check(pod_paged *cache, void *stream);
  * pages held until pod_paged_store and the attention calls write them.  First, window pages whose tokens are all distant for the
  * first new token go back to the pool, for entries with counts[e] > 0.  Then pages are taken, the lowest free page first, in
  * (entry, token) order.  A slot outside the cache, named twice, or that would pass max_context, or a negative count: the call does
- * nothing (flag).  Too few free pages in either pool: nothing is taken and no length changes (flag; window pages that went back stay back).
+ * nothing (flag).  Too few free pages in either pool: nothing is taken and no length changes (flag; window pages that went back stay back:
+ * a last token that still attended one of them is refused from then on, by pod_paged_plan and pod_paged_decode).
  */
 int pod_paged_extend(pod_paged *cache, const int32_t *counts, const int32_t *slots, int n, void *stream);
 
@@ -722,7 +723,8 @@ int pod_paged_prefill(pod_paged *cache, int layer, const void *k, int64_t k_stri
  * Attention of one token per sequence, the last that its slot holds.
  *   k_new, v_new : [n] rows of that token, stored in its page first (by the same launch); both NULL = they are there already
  *   workspace    : dev scratch of pod_paged_workspace_bytes(cfg) bytes, 256-byte aligned; contents undefined afterwards
- *   out          : dev [n][Hq][d].  An empty slot gives zeros; so does a slot outside the cache (flag).
+ *   out          : dev [n][Hq][d].  An empty slot gives zeros; so do a slot outside the cache and, for heads with keys of their own at
+ *                  `layer`, a token whose window pages are gone (flag).
  * POD_ERR_CAPACITY also where n sequences of max_context tokens with all kv heads would pass 2^31 tiles of 32 tokens.
  * Other arguments as in pod_paged_prefill.
  */

@@ -269,6 +269,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
         };
         // rows of a tile: two halves of 16 tokens, each inside one page (the last token's page for a half behind the end)
         struct bases { gbytes k[2], v[2]; };
+        bool lost = false; // an own key that the token attends lies in a window page that is gone (a refused extend may have given it back)
         auto bases_of = [&](int t0, bool dist) {
             bases b;
 #pragma unroll
@@ -276,7 +277,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
                 const int at = min(t0 + 16 * half, n - 1), i = at >> ps_shift;
                 int page = table[i], kpage = (dist || low ? table : wtable)[i];
                 page = (unsigned)page < (unsigned)c.np ? page : 0;
-                kpage = (unsigned)kpage < (unsigned)(dist || low ? c.np : c.nw) ? kpage : 0; // (a window page that is gone: its keys are masked)
+                const bool there = (unsigned)kpage < (unsigned)(dist || low ? c.np : c.nw);
+                lost = lost || (!there && !dist && (at < S || at + 15 >= n - W));
+                kpage = there ? kpage : 0; // (any page: its keys are masked, or nothing of the pair counts)
                 const size_t row = (size_t)(at & (c.ps - 1)) * RB;
                 b.v[half] = vpool + page * page_bytes + row;
                 b.k[half] = (dist ? kpool : wpool) + kpage * page_bytes + row;
@@ -423,6 +426,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
 
         // ---- the four waves' sums become one.  acc[x][i] is O^T[dim VD (4 j + i) + x][head m16]
         l_run = sum_over_16s(l_run);
+        if (lost) { // a maximum above every other, an infinite sum, no values: the entry's row becomes zeros, whoever adds the parts
+            if (lane == 0) atomicOr(c.flag, kPagedBadEntry);
+            m_run = -kLowestLogit;
+            l_run = __builtin_inff();
+#pragma unroll
+            for (int x = 0; x < VD; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         __syncthreads(); // every wave is done with its K tiles (and with the last pair's merge)
         float *const sm = (float *)lds;
         if (m16 < rep) {

@@ -55,3 +55,38 @@ def test_rows_of_several_extends_attend_what_they_should_or_are_refused():
     assert bool((out == 7).all())
     for t, b in zip((p.cache.keys, p.cache.values, p.cache.window_keys), before):
         assert torch.equal(t.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d,held,lost", [(64, 640, True), (64, 641, False), (128, 640, True), (128, 6400, True), (64, 6399, False), (64, 79, False), (64, 80, False), (64, 96, True)])
+def test_a_refused_extend_never_gives_a_held_token_another_answer(d, held, lost, dtype):
+    """W = 65 and pages of 16: the extend's first token no longer needs the page of tokens .. held - 65, the last held one does where that is the page's
+    last.  The answer stays, or the call refuses it; layers whose keys are in context pages go on."""
+    p = Paged(2, 2, 4, 2, d, 16, 65, 2, 8000, 16, 450, 450, dtype, seed=held)
+    p.extend([held - 1, 50], [0, 1])
+    p.prompt([0, 1], [held - 1, 50])
+    p.extend([1], [0])
+    k, v, q = ([p.rows(1, h) for _ in range(2)] for h in (2, 2, 4))
+    for layer in range(2):
+        p._note(layer, [0], [1], k[layer], v[layer])
+        out = p.cache.pod_paged_decode(layer, k[layer], v[layer], q[layer], q[0] if layer else None, p.scale, p.ints([0]))
+        p.check(layer, 0, 1, q[layer], q[0] if layer else None, out)
+    want = out
+    assert not p.extend([8000 - held], [0])
+    p.assert_books()
+    assert bool(_missing(p.model, 0, 1)) == lost
+    both = [torch.cat([t, p.rows(1, 4)]) for t in q]
+    out = p.cache.pod_paged_decode(0, None, None, both[0], None, p.scale, p.ints([0, 1]))
+    p.expect(True)
+    p.check(0, 0, 1, q[0], None, out[:1])
+    out = p.cache.pod_paged_decode(1, None, None, both[1], both[0], p.scale, p.ints([0, 1]))
+    p.expect(not lost)
+    p.check(1, 1, 1, both[1][1:], both[0][1:], out[1:])
+    if lost:
+        assert not out[0].any()
+    else:
+        p.check(1, 0, 1, q[1], q[0], out[:1])
+        alone = p.cache.pod_paged_decode(1, None, None, q[1], q[0], p.scale, p.ints([0]))
+        assert torch.equal(alone, want)
+    p.cache.pod_paged_plan(p.ints([0, 1]), 1, p.ints([0]))
+    p.expect(not lost)
