@@ -671,6 +671,9 @@ int pod_paged_check(pod_paged *cache, void *stream);
  * (entry, token) order.  A slot outside the cache, named twice, or that would pass max_context, or a negative count: the call does
  * nothing (flag).  Too few free pages in either pool: nothing is taken and no length changes (flag; window pages that went back stay back:
  * a last token that still attended one of them is refused from then on, by pod_paged_plan and pod_paged_decode).
+ * A refused call leaves its slots with counts[e] != 0 without room, so that what follows in the same step overwrites nothing that is held: a plan
+ * with more rows of such a slot than later extends made room for is empty (flag), and pod_paged_decode with k_new passes the slot over until
+ * one did.  pod_paged_check lifts this, and so does freeing the slot.
  */
 int pod_paged_extend(pod_paged *cache, const int32_t *counts, const int32_t *slots, int n, void *stream);
 
@@ -721,10 +724,11 @@ int pod_paged_prefill(pod_paged *cache, int layer, const void *k, int64_t k_stri
 
 /*
  * Attention of one token per sequence, the last that its slot holds.
- *   k_new, v_new : [n] rows of that token, stored in its page first (by the same launch); both NULL = they are there already
+ *   k_new, v_new : [n] rows of that token, stored in its page first (by the same launch); both NULL = they are there already.  A slot that
+ *                  got no token since its last one was stored is left out of the call: its last token's rows would be replaced
  *   workspace    : dev scratch of pod_paged_workspace_bytes(cfg) bytes, 256-byte aligned; contents undefined afterwards
- *   out          : dev [n][Hq][d].  An empty slot gives zeros; so do a slot outside the cache and, for heads with keys of their own at
- *                  `layer`, a token whose window pages are gone (flag).
+ *   out          : dev [n][Hq][d].  An empty slot gives zeros; so do a slot outside the cache, for heads with keys of their own at
+ *                  `layer` a token whose window pages are gone (flag), and, with k_new, a slot whose extend was refused.
  * POD_ERR_CAPACITY also where n sequences of max_context tokens with all kv heads would pass 2^31 tiles of 32 tokens.
  * Other arguments as in pod_paged_prefill.
  */

@@ -10,6 +10,7 @@ constexpr int kPagedTileRows = 128;      // (token, query head of the group) row
 struct pod_paged_view {
     char *base;
     int32_t *flag, *lens, *refs, *wrefs, *table, *wtable;
+    int32_t *room;                       // [max_batch] how many of a slot's last tokens may be written: kPagedAnyRoom, or what was made room for since an extend was refused
     int32_t *tickets;                    // [max_batch * Hkv] arrival counters of the decode launches, zero between launches
     int32_t *scratch;                    // fork and compact: see there
     int32_t B, ps, width, np, nw, maxctx, S, W, L, Hq, Hkv, rep, D;
@@ -49,6 +50,7 @@ pod_paged_plan_view pod_paged_plan_at(const void *plan, int rep, int n, int rows
 typedef const __attribute__((address_space(1))) pod_u32x4 *pod_gvec;
 
 int pod_launch_paged_reset(const pod_paged *c, hipStream_t st);
+int pod_launch_paged_clear(const pod_paged *c, hipStream_t st); // the flag, and what refused extends left in room
 int pod_launch_paged_extend(const pod_paged *c, const int32_t *counts, const int32_t *slots, int n, hipStream_t st);
 int pod_launch_paged_fork(const pod_paged *c, const int32_t *src, const int32_t *dst, int n, hipStream_t st);
 int pod_launch_paged_free(const pod_paged *c, const int32_t *slots, int n, hipStream_t st);
@@ -70,6 +72,7 @@ int pod_launch_paged_decode(const pod_paged *c, const pod_paged_call &a, hipStre
 size_t pod_paged_decode_workspace(const pod_layout &ly);
 pod_paged_heads pod_paged_make_heads(const pod_paged *c, int layer);
 
+constexpr int kPagedAnyRoom = 0x7fffffff;
 constexpr int kPagedPlanValid = 0x706c616e; // head.valid of a plan that was made and not refused
 
 enum { kPagedBadEntry = 1, kPagedNoPages = 2, kPagedBadPlan = 4 }; // bits of the sticky flag

@@ -14,7 +14,7 @@ namespace {
 struct paged_layout {
     pod_layout ly;
     pod_paged_regions r;
-    size_t off_flag, off_tickets, off_scratch, total;
+    size_t off_flag, off_room, off_tickets, off_scratch, total;
 };
 
 // scratch of fork and compact: see pod_paged_kernels.hip
@@ -46,6 +46,7 @@ int make_paged_layout(const pod_paged_config *cfg, paged_layout *pl)
     const size_t np = cfg->num_pages, nw = cfg->num_window_pages, row = (size_t)ly.D * 2, table = (size_t)ly.B * r.table_width * 4;
     size_t off = 0;
     pl->off_flag = off; off += 256;
+    pl->off_room = off; off = align_up(off + (size_t)ly.B * 4, 256);
     pl->off_tickets = off; off = align_up(off + (size_t)ly.B * ly.Hkv * 4, 256);
     pl->off_scratch = off; off = align_up(off + scratch_ints(cfg) * 4, 256);
     r.state = off;
@@ -225,6 +226,7 @@ extern "C" int pod_paged_init(const pod_paged_config *cfg, void *dev_buf, size_t
     pod_paged_view &v = c->v;
     v.base = (char *)dev_buf;
     v.flag = (int32_t *)(v.base + pl.off_flag);
+    v.room = (int32_t *)(v.base + pl.off_room);
     v.tickets = (int32_t *)(v.base + pl.off_tickets);
     v.scratch = (int32_t *)(v.base + pl.off_scratch);
     v.lens = (int32_t *)(v.base + pl.r.lens);
@@ -256,11 +258,10 @@ extern "C" int pod_paged_check(pod_paged *cache, void *stream)
     if (!cache) return pod_fail(POD_ERR_INVALID_ARG, "cache is NULL");
     const hipStream_t st = (hipStream_t)stream;
     int32_t flag = 0;
-    const int32_t zero = 0;
     POD_HIP_TRY(hipMemcpyAsync(&flag, cache->v.flag, sizeof flag, hipMemcpyDeviceToHost, st));
     POD_HIP_TRY(hipStreamSynchronize(st));
     if (!flag) return POD_OK;
-    POD_HIP_TRY(hipMemcpyAsync(cache->v.flag, &zero, sizeof zero, hipMemcpyHostToDevice, st));
+    if (const int rc = pod_launch_paged_clear(cache, st)) return rc;
     POD_HIP_TRY(hipStreamSynchronize(st));
     return pod_fail(POD_ERR_STATE, "a call was refused on the device:%s%s%s", flag & kPagedBadEntry ? " an entry that does not fit the cache's state;" : "",
                     flag & kPagedNoPages ? " too few free pages;" : "", flag & kPagedBadPlan ? " rows that do not fit the slots' tokens;" : "");

@@ -148,6 +148,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
         const bool bad = slot < 0 || slot >= c.B;
         if (bad && blockIdx.x == 0) atomicOr(c.flag, kPagedBadEntry);
         n = bad ? 0 : c.lens[slot];
+        if (p.k && !bad && c.room[slot] < 1) n = 0; // (room for the new token was refused: the last token is another one)
         if (n < 0 || n > c.maxctx) n = 0;
         return p.low_heads * (p.low_heads ? count_of(n, S, W, true) : 0) + (hkv - p.low_heads) * (p.low_heads < hkv ? count_of(n, S, W, false) : 0);
     };

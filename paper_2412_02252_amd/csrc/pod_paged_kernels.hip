@@ -117,12 +117,19 @@ __global__ void paged_reset_kernel(pod_paged_view c)
     for (size_t i = at; i < table; i += step) { c.table[i] = -1; c.wtable[i] = -1; }
     for (size_t i = at; i < (size_t)c.np; i += step) c.refs[i] = 0;
     for (size_t i = at; i < (size_t)c.nw; i += step) c.wrefs[i] = 0;
-    for (size_t i = at; i < (size_t)c.B; i += step) c.lens[i] = 0;
+    for (size_t i = at; i < (size_t)c.B; i += step) { c.lens[i] = 0; c.room[i] = kPagedAnyRoom; }
     for (size_t i = at; i < (size_t)c.B * c.Hkv; i += step) c.tickets[i] = 0;
     if (at == 0) *c.flag = 0;
 }
 
-// ---- extend
+__global__ __launch_bounds__(kBook) void paged_clear_kernel(pod_paged_view c)
+{
+    if ((int)threadIdx.x < c.B) c.room[threadIdx.x] = kPagedAnyRoom;
+    if (threadIdx.x == 0) *c.flag = 0;
+}
+
+// ---- extend.  A refused one leaves its entries without room (c.room): the length has not grown, so what follows in the same step would
+// write its rows over tokens that are held, in pages that other slots may share.
 
 __global__ __launch_bounds__(kBook) void paged_extend_kernel(pod_paged_view c, const int32_t *counts, const int32_t *slots, int n)
 {
@@ -131,17 +138,21 @@ __global__ __launch_bounds__(kBook) void paged_extend_kernel(pod_paged_view c, c
     const int e = threadIdx.x;
     if (e < kPagedMaxBatch / 32) seen[e] = 0;
     __syncthreads();
-    int slot = 0, len = 0, count = 0, bad = 0;
+    int slot = 0, len = 0, count = 0, bad = 0, room = 0;
+    bool inside = false;
     if (e < n) {
         slot = slots ? slots[e] : e;
         count = counts[e];
-        bad = slot < 0 || slot >= c.B || count < 0;
+        inside = slot >= 0 && slot < c.B;
+        bad = !inside || count < 0;
         if (!bad) {
             len = c.lens[slot];
+            room = c.room[slot];
             bad = mark(seen, slot) || len < 0 || len > c.maxctx || count > c.maxctx - len;
         }
     }
     if (__syncthreads_or(bad)) {
+        if (inside && count != 0) c.room[slot] = 0;
         if (e == 0) atomicOr(c.flag, kPagedBadEntry);
         return;
     }
@@ -179,6 +190,7 @@ __global__ __launch_bounds__(kBook) void paged_extend_kernel(pod_paged_view c, c
         pages.count();
         wpages.count();
         if (pages.total < total || (c.nw && wpages.total < total)) {
+            if (inside && count > 0) c.room[slot] = 0;
             if (e == 0) atomicOr(c.flag, kPagedNoPages);
             return;
         }
@@ -195,7 +207,10 @@ __global__ __launch_bounds__(kBook) void paged_extend_kernel(pod_paged_view c, c
         pages.take(total, [&](int r, int page) { *entry_of(c.table, r) = page; c.refs[page] = 1; });
         if (c.nw) wpages.take(total, [&](int r, int page) { *entry_of(c.wtable, r) = page; c.wrefs[page] = 1; });
     }
-    if (e < n) c.lens[slot] = len + count;
+    if (e < n) {
+        c.lens[slot] = len + count;
+        if (room != kPagedAnyRoom) c.room[slot] = room + count; // (never above the length)
+    }
 }
 
 // ---- fork.  scratch: [0] entries (0: refused), from 8 on per entry: context page from, to, window page from, to (-1: none)
@@ -208,13 +223,14 @@ __global__ __launch_bounds__(kBook) void paged_fork_plan_kernel(pod_paged_view c
     free_list pages(c.refs, c.np), wpages(c.wrefs, c.nw);
     if (e < kPagedMaxBatch / 32) is_src[e] = is_dst[e] = 0;
     __syncthreads();
-    int s = 0, d = 0, bad = 0, len = 0;
+    int s = 0, d = 0, bad = 0, len = 0, room = 0;
     if (e < n) {
         s = src[e];
         d = dst[e];
         bad = s < 0 || s >= c.B || d < 0 || d >= c.B;
         if (!bad) {
             len = c.lens[s];
+            room = c.room[s];
             mark(is_src, s);
             bad = mark(is_dst, d) || c.lens[d] != 0 || len < 0 || len > c.maxctx;
         }
@@ -256,7 +272,7 @@ __global__ __launch_bounds__(kBook) void paged_fork_plan_kernel(pod_paged_view c
         pages.take(total, [&](int r, int page) { give(r, page, c.table, c.refs, 1); });
         if (c.nw) wpages.take(total, [&](int r, int page) { give(r, page, c.wtable, c.wrefs, 3); });
     }
-    if (e < n) c.lens[d] = len;
+    if (e < n) { c.lens[d] = len; c.room[d] = room; }
 }
 
 // blockIdx.y: entry; blockIdx.x: 0 the tables, then one stream each (key, value, window)
@@ -313,7 +329,7 @@ __global__ __launch_bounds__(256) void paged_free_kernel(pod_paged_view c, const
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) c.lens[s] = 0;
+    if (threadIdx.x == 0) { c.lens[s] = 0; c.room[s] = kPagedAnyRoom; }
 }
 
 // ---- compact.  scratch: [0] context moves, [1] window moves, [2], [3] pages in use; from 8 on np entries: the r-th move's page from at
@@ -418,7 +434,7 @@ __global__ __launch_bounds__(kBook) void paged_plan_kernel(pod_paged_view c, con
         bad = slot < 0 || slot >= c.B || lo < 0 || hi < lo || hi > rows || (e == 0 && lo != 0) || (e == n - 1 && hi != rows);
         if (!bad) {
             len = c.lens[slot];
-            bad = mark(seen, slot) || len < hi - lo || len > c.maxctx;
+            bad = mark(seen, slot) || len < hi - lo || len > c.maxctx || c.room[slot] < hi - lo;
         }
         if (c.nw && !bad && hi > lo) {
             // What the rows attend by their own layers' keys starts at the first row's window (sink pages never go back).  Pages go back oldest
@@ -524,6 +540,13 @@ __global__ __launch_bounds__(256) void paged_store_kernel(store_params a)
 int pod_launch_paged_reset(const pod_paged *c, hipStream_t st)
 {
     paged_reset_kernel<<<256, 256, 0, st>>>(c->v);
+    POD_HIP_TRY(hipGetLastError());
+    return POD_OK;
+}
+
+int pod_launch_paged_clear(const pod_paged *c, hipStream_t st)
+{
+    paged_clear_kernel<<<1, kBook, 0, st>>>(c->v);
     POD_HIP_TRY(hipGetLastError());
     return POD_OK;
 }

@@ -90,3 +90,175 @@ def test_a_refused_extend_never_gives_a_held_token_another_answer(d, held, lost,
         assert torch.equal(alone, want)
     p.cache.pod_paged_plan(p.ints([0, 1]), 1, p.ints([0]))
     p.expect(not lost)
+
+
+def _pools(p):
+    return [t.clone().view(torch.int16) for t in (p.cache.keys, p.cache.values, p.cache.window_keys)]
+
+
+def _unchanged(p, before):
+    return all(torch.equal(t.view(torch.int16), b) for t, b in zip((p.cache.keys, p.cache.values, p.cache.window_keys), before))
+
+
+def _refused(p, counts, slots):
+    """An extend that the model refuses; nobody asks the cache."""
+    p.cache.pod_paged_extend(p.ints(counts), p.ints(slots))
+    assert not p.model.extend(counts, slots)
+
+
+def _try_step(p, slots):
+    """Both layers' calls of a step, rows that must go nowhere: the outputs."""
+    n, outs, qs = len(slots), [], None
+    for layer in range(p.L):
+        k, v, q = p.rows(n, p.Hkv), p.rows(n, p.Hkv), p.rows(n, p.Hq)
+        outs.append(p.cache.pod_paged_decode(layer, k, v, q, qs, p.scale, p.ints(slots)))
+        qs = q
+    return outs
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("shared", [64, 70])
+def test_a_step_after_a_refused_extend_overwrites_nothing(shared, many):
+    """Three samples of a prompt, at a page's border or inside a page; no page is left for the next token."""
+    slots = 70 if many else 4                                    # (more than 64 entries: the list that is summed up in LDS)
+    p = Paged(2, 2, 4, 2, 64, 5, 30, slots, 2000, 16, 9 + slots, 9 + slots, seed=shared)
+    p.extend([shared], [1])
+    p.prompt([1], [shared])
+    p.fork([1, 1], [0, 3])
+    if shared % 16:
+        fill = 16 - shared % 16
+        p.extend([fill] * 3, [1, 0, 3])
+        p.prompt([1, 0, 3], [fill] * 3)
+    free = min(p.model.refs[k].count(0) for k in "cw")
+    assert p.extend([16 * (free - 1)], [2])
+    p.prompt([2], [16 * (free - 1)])
+    live = [3, 0, 1] + list(range(4, slots))
+    before = _pools(p)
+    for _ in range(2):
+        _refused(p, [1] * len(live), live)
+        assert not any(t.any() for t in _try_step(p, live))
+        p.cache.pod_paged_plan(p.ints([0, 1]), 1, p.ints([3]))
+    assert _unchanged(p, before)
+    p.expect(False)
+    p.assert_books()
+    p.free([2])
+    _refused(p, [3000], [0])                                     # one that was refused and then got room, unasked in between
+    some = [3, 0, 1] if many else [3, 0, 1, 2]
+    p.cache.pod_paged_extend(p.ints([1] * len(some)), p.ints(some))
+    assert p.model.extend([1] * len(some), some)
+    queries = []
+    for layer in range(2):
+        k, v, q = p.rows(len(some), 2), p.rows(len(some), 2), p.rows(len(some), 4)
+        queries.append(q)
+        p._note(layer, some, [1] * len(some), k, v)
+        out = p.cache.pod_paged_decode(layer, k, v, q, queries[0] if layer else None, p.scale, p.ints(some))
+        for e, s in enumerate(some):
+            p.check(layer, s, 1, q[e:e + 1], queries[0][e:e + 1] if layer else None, out[e:e + 1])
+    p.expect(False)
+    p.extend([1], [0])
+    p.step([0])
+    p.assert_books()
+
+
+def test_a_plan_after_a_refused_extend_has_the_later_rooms_only():
+    p = Paged(2, 2, 4, 2, 64, 5, 30, 3, 400, 16, 20, 20, seed=8)
+    p.extend([100, 40], [0, 1])
+    p.prompt([0, 1], [100, 40])
+    before = _pools(p)
+    _refused(p, [60, 200], [0, 1])
+    for rows in (1, 20, 40):
+        plan = p.cache.pod_paged_plan(p.ints([0, rows]), rows, p.ints([1]))
+        p.cache.pod_paged_store(0, p.rows(rows, 2), p.rows(rows, 2), plan)
+    assert _unchanged(p, before)
+    p.cache.pod_paged_extend(p.ints([7, 9]), p.ints([1, 0]))     # accepted, but nobody has asked about the refusal yet
+    assert p.model.extend([7, 9], [1, 0])
+    before = _pools(p)
+    plan = p.cache.pod_paged_plan(p.ints([0, 8, 17]), 17, p.ints([1, 0]))
+    p.cache.pod_paged_store(0, p.rows(17, 2), p.rows(17, 2), plan)
+    assert _unchanged(p, before)
+    p.expect(False)
+    _refused(p, [400, 1], [0, 1])
+    p.expect(False)                                              # asked: from here on every row may be written again, as long as it is there
+    p.prompt([1, 0], [7, 9])
+    p.extend([3, 2], [0, 1])
+    p.prompt([0, 1], [3, 2], stored_first=True)
+    p.assert_books()
+
+
+def test_a_refused_extend_holds_back_its_own_entries_only():
+    p = Paged(2, 2, 4, 2, 64, 5, 30, 5, 400, 16, 20, 20, seed=9)
+    p.extend([30, 31, 32], [0, 1, 2])
+    p.prompt([0, 1, 2], [30, 31, 32])
+    for counts, slots in (([400, 0, 1], [1, 0, 2]), ([1, 1], [1, 9]), ([-1], [1]), ([1, 1], [1, 1])):
+        p.cache.pod_paged_extend(p.ints([1]), p.ints([0]))
+        assert p.model.extend([1], [0])
+        before = _pools(p)
+        _refused(p, counts, slots)
+        assert not any(t.any() for t in _try_step(p, [1]))
+        assert _unchanged(p, before)
+        queries = []
+        for layer in range(2):                                   # slot 0 has its token
+            k, v, q = p.rows(1, 2), p.rows(1, 2), p.rows(1, 4)
+            queries.append(q)
+            p._note(layer, [0], [1], k, v)
+            out = p.cache.pod_paged_decode(layer, k, v, q, queries[0] if layer else None, p.scale, p.ints([0]))
+            p.check(layer, 0, 1, q, queries[0] if layer else None, out)
+        p.expect(False)
+    _refused(p, [400], [1])
+    p.cache.pod_paged_fork(p.ints([1]), p.ints([3]))             # a sample of a slot without room has none either
+    p.model.fork([1], [3])
+    before = _pools(p)
+    assert not any(t.any() for t in _try_step(p, [3, 1]))
+    assert _unchanged(p, before)
+    p.cache.pod_paged_free(p.ints([1, 3]))                       # a freed slot begins anew
+    p.model.free([1, 3])
+    p.k[1], p.v[1] = [[], []], [[], []]
+    p.cache.pod_paged_extend(p.ints([20]), p.ints([1]))
+    assert p.model.extend([20], [1])
+    p.expect(False)
+    p.prompt([1], [20])
+    p.assert_books()
+
+
+def test_replays_of_a_step_that_finds_no_page():
+    """One graph: room for a token, both layers.  Replays without a free page change nothing; once there are pages it goes on, unasked."""
+    p = Paged(2, 2, 4, 2, 64, 5, 30, 3, 400, 16, 14, 14, seed=10)
+    p.extend([31, 60, 80], [0, 1, 2])
+    p.prompt([0, 1, 2], [31, 60, 80])
+    slots, one = p.ints([0, 1]), p.ints([1, 1])
+    k, v, q = ([p.rows(2, h) for _ in range(2)] for h in (2, 2, 4))
+    outs = [torch.empty_like(t) for t in q]
+
+    def step():
+        p.cache.pod_paged_extend(one, slots)
+        for layer in range(2):
+            p.cache.pod_paged_decode(layer, k[layer], v[layer], q[layer], q[0] if layer else None, p.scale, slots, out=outs[layer])
+
+    def replayed(run):
+        for t in k + v + q:
+            t.copy_(torch.randn(t.shape, generator=p.gen).to(p.dtype))
+        before = _pools(p)
+        run()
+        ok = p.model.extend([1, 1], [0, 1])
+        for layer in range(2):
+            if ok:
+                p._note(layer, [0, 1], [1, 1], k[layer], v[layer])
+                for s in range(2):
+                    p.check(layer, s, 1, q[layer][s:s + 1], q[0][s:s + 1] if layer else None, outs[layer][s:s + 1])
+            else:
+                assert not outs[layer].any()
+        assert ok or _unchanged(p, before)
+        return ok
+
+    assert replayed(step)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    answers = [replayed(graph.replay) for _ in range(60)]
+    assert answers[0] and not any(answers[-3:])
+    p.cache.pod_paged_free(p.ints([2]))
+    p.model.free([2])
+    assert all(replayed(graph.replay) for _ in range(20))
+    p.expect(False)
+    p.assert_books()
