@@ -17,14 +17,15 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 __device__ inline int lane_id() { return threadIdx.x & 63; }
 
 // Exclusive prefix sum over the workgroup and the total.  Called by all threads; what they wrote to memory and LDS before, all see after.
-__device__ inline int block_scan(int x, int *total)
+// With a cap < 2^30, and no x above it, sums stop at it: the total is right below it, and so are the prefix sums if it is.
+__device__ __forceinline__ int block_scan(int x, int *total, int cap = 0x7fffffff)
 {
     __shared__ int sums[kBook / 64];
     int incl = x;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
         const int y = __shfl_up(incl, off);
-        if (lane_id() >= off) incl += y;
+        if (lane_id() >= off) incl = min(incl + y, cap);
     }
     __syncthreads(); // (the last call's sums have been read)
     if (lane_id() == 63) sums[threadIdx.x >> 6] = incl;
@@ -32,8 +33,8 @@ __device__ inline int block_scan(int x, int *total)
     int before = 0, all = 0;
     for (int w = 0; w < (int)blockDim.x / 64; ++w) {
         const int s = sums[w];
-        if (w < (int)threadIdx.x >> 6) before += s;
-        all += s;
+        if (w < (int)threadIdx.x >> 6) before = min(before + s, cap);
+        all = min(all + s, cap);
     }
     *total = all;
     return before + incl - x;
@@ -157,11 +158,12 @@ __global__ __launch_bounds__(kBook) void paged_extend_kernel(pod_paged_view c, c
         return;
     }
     slot_of[e] = slot;
-    const int have = (len + c.ps - 1) / c.ps, need = count > 0 ? (len + count + c.ps - 1) / c.ps - have : 0;
+    // (no more than one page above the pool: 1024 entries may want 2^24 pages each, and their sum stops there too)
+    const int have = (len + c.ps - 1) / c.ps, need = count > 0 ? min((len + count + c.ps - 1) / c.ps - have, c.np + 1) : 0;
     first[e] = have;
     held_of[e] = count > 0 ? len : 0;
     int total;
-    before[e] = block_scan(need, &total);
+    before[e] = block_scan(need, &total, c.np + 1);
     if (e == 0) before[kBook] = total;
     __syncthreads();
     if (c.nw) {

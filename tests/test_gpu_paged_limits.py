@@ -3,7 +3,8 @@ a type's range."""
 import pytest
 import torch
 
-from pagedcase import Paged
+import paper_2412_02252_amd as pod
+from pagedcase import DEV, Paged
 
 pytestmark = pytest.mark.gpu
 
@@ -262,3 +263,27 @@ def test_replays_of_a_step_that_finds_no_page():
     assert all(replayed(graph.replay) for _ in range(20))
     p.expect(False)
     p.assert_books()
+
+
+@pytest.mark.parametrize("entries,last", [(128, 1 << 28), (129, 16), (257, 16)])
+def test_more_pages_than_32_bits_count_are_too_few(entries, last):
+    """2^24 pages for each entry but the last: 2^31 in all, 2^31 and one, 2^32 and one; tables of 8 GB and more."""
+    free, total = torch.cuda.mem_get_info()
+    tokens = 1 << 28
+    if free < entries * tokens // 16 * 4 * 2 + (4 << 30):
+        pytest.skip("the tables do not fit")
+    cache = pod.PagedCache(pod.make_paged_config(1, 1, 1, 1, 64, 0, 16, entries, tokens, 16, 20, 0), DEV)
+    counts = torch.full((entries,), tokens, dtype=torch.int32, device=DEV)
+    counts[-1] = last
+    before = cache.lens.clone(), cache.page_refs.clone()
+    cache.pod_paged_extend(counts)
+    with pytest.raises(pod.PodError) as e:
+        cache.pod_paged_check()
+    assert e.value.code == pod.binding.ERR_STATE and "too few free pages" in str(e.value)
+    assert torch.equal(cache.lens, before[0]) and torch.equal(cache.page_refs, before[1])
+    counts[:] = 0
+    counts[[0, entries - 1]] = torch.tensor([100, 200], dtype=torch.int32, device=DEV)   # 7 + 13 pages: all there are
+    cache.pod_paged_extend(counts)
+    cache.pod_paged_check()
+    assert cache.lens[[0, entries - 1]].tolist() == [100, 200] and bool((cache.page_refs == 1).all())
+    assert cache.page_table[0, :8].tolist() == [*range(7), -1] and cache.page_table[entries - 1, :14].tolist() == [*range(7, 20), -1]
