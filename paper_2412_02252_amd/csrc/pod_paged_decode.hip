@@ -393,11 +393,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
             }
             float top = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
             top = max_over_16s(top);
-            const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new), shift = m_new - T::spare(0.f);
             float part = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                sc[i] = __builtin_amdgcn_exp2f(sc[i] - m_new);
+                sc[i] = __builtin_amdgcn_exp2f(sc[i] - shift);
                 part += sc[i];
             }
             l_run = l_run * alpha + part;

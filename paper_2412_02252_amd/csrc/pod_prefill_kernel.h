@@ -139,7 +139,7 @@ __device__ inline float pair_sum(float x)
 // the next iteration, which moves the reference maximum if the tile exceeds it by more than 2^8
 // and rescales the accumulators (rare).  Masked logits are -infinity (exponential 0 whatever the
 // reference); every wave walks every tile of its workgroup.  The row sum adds the bf16-rounded
-// probabilities (add_four), i.e. exactly the weights the PV product uses.
+// probabilities (sum_four), i.e. exactly the weights the PV product uses.
 //
 // Data movement uses no registers: K and V tiles go from global memory straight into LDS
 // (global_load_lds_dwordx4: each wave instruction fills 1 KB of consecutive LDS, lane l its 16
@@ -597,7 +597,7 @@ __global__ __launch_bounds__(256 * KS, 2) void prefill_kernel(typename params_of
             m_ref = mx_next;
         }
         if (__builtin_expect(ph_a && !ph_b, 0)) load_q(false); // the next tile is the first of the own-key phase
-        const float mr = m_ref;
+        const float mr = m_ref - E::spare(kLazy); // (weights reach 2^kLazy)
         f32x4 lsum = {0.f, 0.f, 0.f, 0.f}; // this tile's row sum, four times
         __builtin_amdgcn_sched_barrier(0);
         static_for<NS>([&](auto ic) {

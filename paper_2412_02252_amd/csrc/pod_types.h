@@ -21,7 +21,12 @@ typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 // (v_dot2c_f32_bf16 in their place does not run beside the matrix pipe as the other vector instructions do: synthetic loops,
 // two waves per SIMD, 14 ns per 32x32x16 MFMA alone and with four v_fma_f32 beside it, 22 with two dot products; the whole mix of a prefill
 // iteration 17.5 -> 17.1 ns per MFMA, against 18.4 with the pairs taken apart and added.  16384 tokens x 32/8 heads x 128 4132 -> 4000 us.)
+//
+// spare(top): log2 of the factor that softmax weights up to 2^top are packed with; sums carry it too, the division takes it out.  bf16 has the
+// exponents of 32 bits and needs none.  fp16 ends at 65504 and rounds what is below 2^-14 to steps of 2^-24: without a factor, 131072 tokens whose
+// weights are 2^-26 of the largest would vanish with 2^-9 of the result; with weights up to 2^15 what vanishes is 2^-40 - top of it each.
 struct type_bf16 {
+    static constexpr float spare(float) { return 0.f; }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -40,6 +45,7 @@ struct type_bf16 {
     static __device__ __forceinline__ float high(unsigned v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
 };
 struct type_fp16 {
+    static constexpr float spare(float top) { return 15.f - top; }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);

@@ -1,5 +1,7 @@
 """GPU: the paged cache where a call meets less than it needs: window pages that are gone, rooms that were refused, sums past 32 bits, weights below
 a type's range."""
+import math
+
 import pytest
 import torch
 
@@ -287,3 +289,49 @@ def test_more_pages_than_32_bits_count_are_too_few(entries, last):
     cache.pod_paged_check()
     assert cache.lens[[0, entries - 1]].tolist() == [100, 200] and bool((cache.page_refs == 1).all())
     assert cache.page_table[0, :8].tolist() == [*range(7), -1] and cache.page_table[entries - 1, :14].tolist() == [*range(7, 20), -1]
+
+
+@pytest.mark.parametrize("bits", [20.0, 26.0, 30.0])
+@pytest.mark.parametrize("where", ["first", "own"])
+def test_many_small_weights_beside_a_large_one(where, bits):
+    """fp16: 120000 keys whose weights are about 2^-bits of one key's, which has the value 0: the result is theirs alone.
+
+    An element differs by its rounding, eps / 2 |o| or half a step of 2^-24; by that of the weights, once in the product and once in the sum that divides,
+    2 eps / 2 sum_j w_j |v_j|; by weights whose packed form is below the type's normal range: off by half of 2^-24 of the largest weight's share of its
+    packed form, which is at least 2^7: sum_j |v_j| 2^-32 / l; and by 32-bit sums, 2^-24 a step over n / 16 steps of products and of the sum, and of logits of
+    2^5 over 64 products: 2 (n / 16 + 2^11) 2^-24 sum_j w_j |v_j|."""
+    n, hq, d = 120000, 2, 64
+    p = Paged(1, 1, hq, 1, d, 4, 64, 1, n + 10, 256, 500, 0, torch.float16)
+    k, v = 0.2 * torch.randn((n + 3, 1, d), generator=p.gen), 1 + torch.randn((n + 3, 1, d), generator=p.gen)
+    big = [0] if where == "first" else list(range(n, n + 3))
+    k[:, :, 0] = 0
+    k[big] = 0
+    k[big, :, 0] = bits * math.log(2)                            # q k scale = bits ln 2
+    v[big] = 0
+    q = 0.5 * torch.randn((3, hq, d), generator=p.gen)
+    q[:, :, 0] = 1 / p.scale
+    k, v, q = (t.half() for t in (k, v, q))
+    half = torch.finfo(torch.float16).eps / 2
+
+    def close(out, rows, last):                                  # tokens .. last
+        i, out = torch.arange(last + 1 - rows, last + 1)[:, None], out.cpu().double()
+        for h in range(hq):
+            a = q[last + 1 - rows - n:last + 1 - n, h].double() @ k[:last + 1, 0].double().T * p.scale
+            a = torch.where(torch.arange(last + 1)[None] <= i, a, -math.inf)
+            w = torch.exp(a - a.amax(-1, keepdim=True))
+            l, vd = w.sum(-1, keepdim=True), v[:last + 1, 0].double()
+            want, size = w @ vd / l, w @ vd.abs() / l
+            tol = half * (want.abs() + 2 * size) + 2.0 ** -25 + vd.abs().sum(0) * 2.0 ** -32 / l + 2 * (last / 16 + 2 ** 11) * 2.0 ** -24 * size
+            err = (out[:, h] - want).abs()
+            assert bool((err <= tol).all()), (rows, h, float((err / tol).max()), float(want.abs().mean()), float(out[:, h].abs().mean()))
+
+    dev = [t.to(DEV) for t in (k, v, q)]
+    c = p.cache
+    c.pod_paged_extend(p.ints([n]))
+    c.pod_paged_store(0, dev[0][:n], dev[1][:n], c.pod_paged_plan(p.ints([0, n]), n))
+    c.pod_paged_extend(p.ints([2]))
+    plan = c.pod_paged_plan(p.ints([0, 2]), 2)
+    close(c.pod_paged_prefill(0, dev[0][n:n + 2], dev[1][n:n + 2], dev[2][:2], None, plan, p.scale), 2, n + 1)
+    c.pod_paged_extend(p.ints([1]))
+    close(c.pod_paged_decode(0, dev[0][n + 2:], dev[1][n + 2:], dev[2][2:], None, p.scale), 1, n + 2)
+    c.pod_paged_check()
