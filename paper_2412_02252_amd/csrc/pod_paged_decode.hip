@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m16 = lane & 15, j = lane >> 4;
     const int S = c.S, W = c.W, rep = c.rep, hkv = c.Hkv;
     // The arguments lie on several cache lines; without this they are fetched one after the other, each where it is first used.
-    asm volatile("" ::"s"(p.slots), "s"(c.lens), "s"(c.table), "s"(c.B), "s"(c.maxctx), "s"(S), "s"(W), "s"(hkv), "s"(p.n), "s"(p.low_heads), "s"(p.k_stride), "s"(p.part), "s"(p.heads.window[0]));
+    asm volatile("" ::"s"(p.slots), "s"(c.lens), "s"(c.room), "s"(c.table), "s"(c.B), "s"(c.maxctx), "s"(S), "s"(W), "s"(hkv), "s"(p.n), "s"(p.low_heads), "s"(p.k_stride), "s"(p.part), "s"(p.heads.window[0]));
 
     // ---- the list: tiles up to and with each sequence's.  Of up to 64 sequences every wave keeps them in a lane each, without a barrier; more
     // are summed up in LDS.
@@ -147,8 +147,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
         slot = p.slots ? p.slots[e] : e;
         const bool bad = slot < 0 || slot >= c.B;
         if (bad && blockIdx.x == 0) atomicOr(c.flag, kPagedBadEntry);
-        n = bad ? 0 : c.lens[slot];
-        if (p.k && !bad && c.room[slot] < 1) n = 0; // (room for the new token was refused: the last token is another one)
+        const int at = bad ? 0 : slot, held = c.lens[at], room = c.room[at]; // (both under way at once)
+        n = bad || (p.k && room < 1) ? 0 : held; // (room for the new token was refused: the last token is another one)
         if (n < 0 || n > c.maxctx) n = 0;
         return p.low_heads * (p.low_heads ? count_of(n, S, W, true) : 0) + (hkv - p.low_heads) * (p.low_heads < hkv ? count_of(n, S, W, false) : 0);
     };
@@ -278,9 +278,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged_decode_kernel(decode_par
                 const int at = min(t0 + 16 * half, n - 1), i = at >> ps_shift;
                 int page = table[i], kpage = (dist || low ? table : wtable)[i];
                 page = (unsigned)page < (unsigned)c.np ? page : 0;
-                const bool there = (unsigned)kpage < (unsigned)(dist || low ? c.np : c.nw);
-                lost = lost || (!there && !dist && (at < S || at + 15 >= n - W));
-                kpage = there ? kpage : 0; // (any page: its keys are masked, or nothing of the pair counts)
+                if (__builtin_expect((unsigned)kpage >= (unsigned)(dist || low ? c.np : c.nw), 0)) {
+                    asm volatile(""); // (keeps this a branch)
+                    lost = lost || (!dist && (at < S || at + 15 >= n - W));
+                    kpage = 0;       // any page: its keys are masked, or nothing of the pair counts
+                }
                 const size_t row = (size_t)(at & (c.ps - 1)) * RB;
                 b.v[half] = vpool + page * page_bytes + row;
                 b.k[half] = (dist ? kpool : wpool) + kpage * page_bytes + row;

@@ -158,12 +158,12 @@ __global__ __launch_bounds__(kBook) void paged_extend_kernel(pod_paged_view c, c
         return;
     }
     slot_of[e] = slot;
-    // (no more than one page above the pool: 1024 entries may want 2^24 pages each, and their sum stops there too)
+    // (no more than one page above the pool: 1024 entries may want 2^24 pages each; where even so the sum could pass 32 bits it stops there too, for 0.3 us)
     const int have = (len + c.ps - 1) / c.ps, need = count > 0 ? min((len + count + c.ps - 1) / c.ps - have, c.np + 1) : 0;
     first[e] = have;
     held_of[e] = count > 0 ? len : 0;
     int total;
-    before[e] = block_scan(need, &total, c.np + 1);
+    before[e] = (int64_t)n * (c.np + 1) > 0x7fffffff ? block_scan(need, &total, c.np + 1) : block_scan(need, &total);
     if (e == 0) before[kBook] = total;
     __syncthreads();
     if (c.nw) {

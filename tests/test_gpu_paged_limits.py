@@ -335,3 +335,23 @@ def test_many_small_weights_beside_a_large_one(where, bits):
     c.pod_paged_extend(p.ints([1]))
     close(c.pod_paged_decode(0, dev[0][n + 2:], dev[1][n + 2:], dev[2][2:], None, p.scale), 1, n + 2)
     c.pod_paged_check()
+
+
+def test_sums_stop_above_a_pool_of_millions_of_pages():
+    """1024 entries of 2^21 pages each, as many as the pool has in all: 2^31."""
+    free, total = torch.cuda.mem_get_info()
+    if free < 50 << 30:
+        pytest.skip("the tables and pools do not fit")
+    tokens, pages = 1 << 25, 1 << 21
+    cache = pod.PagedCache(pod.make_paged_config(1, 1, 1, 1, 64, 0, 16, 1024, tokens, 16, pages, 0), DEV)
+    counts = torch.full((1024,), tokens, dtype=torch.int32, device=DEV)
+    cache.pod_paged_extend(counts)
+    with pytest.raises(pod.PodError) as e:
+        cache.pod_paged_check()
+    assert e.value.code == pod.binding.ERR_STATE and "too few free pages" in str(e.value)
+    assert not cache.lens.any() and not cache.page_refs.any()
+    counts[1:] = 0
+    cache.pod_paged_extend(counts)                               # all of them for one
+    cache.pod_paged_check()
+    assert int(cache.lens[0]) == tokens and bool((cache.page_refs == 1).all())
+    assert torch.equal(cache.page_table[0], torch.arange(pages, dtype=torch.int32, device=DEV)) and bool((cache.page_table[1:3] == -1).all())
