@@ -684,7 +684,7 @@ class PagedCache:
         if not t.is_cuda or t.dtype != self.dtype or t.shape != (n, heads, d):
             raise ValueError(f"expected a CUDA {self.dtype} tensor of shape {(n, heads, d)}, got {t.device.type} {t.dtype} {tuple(t.shape)}")
         s = t.stride()
-        if n and (s[2] != 1 or s[1] != d):
+        if n and (s[2] != 1 or (heads > 1 and s[1] != d)):
             raise ValueError("a token's heads must be contiguous")
         return t.data_ptr(), s[0] if n > 1 else max(s[0], heads * d) // 8 * 8
 

@@ -355,3 +355,20 @@ def test_sums_stop_above_a_pool_of_millions_of_pages():
     cache.pod_paged_check()
     assert int(cache.lens[0]) == tokens and bool((cache.page_refs == 1).all())
     assert torch.equal(cache.page_table[0], torch.arange(pages, dtype=torch.int32, device=DEV)) and bool((cache.page_table[1:3] == -1).all())
+
+
+@pytest.mark.parametrize("n", [1, 5])
+def test_rows_of_one_head_may_have_any_head_stride(n):
+    """A token's only head is contiguous whatever the stride between heads that are not there."""
+    p = Paged(1, 1, 1, 1, 64, 4, 50, n, 100, 16, 2 * n, 0)
+    p.extend([1] * n, list(range(n)))
+    k, v, q = (p.rows(n, 1) for _ in range(3))
+    p._note(0, list(range(n)), [1] * n, k, v)
+    turned = [t.as_strided((n, 1, 64), (64, 64 * n + 8, 1)) for t in (k, v, q)]
+    out = p.cache.pod_paged_decode(0, *turned, None, p.scale)
+    for e in range(n):
+        p.check(0, e, 1, q[e:e + 1], None, out[e:e + 1])
+    plan = p.cache.pod_paged_plan(p.ints(list(range(n + 1))), n)
+    p.cache.pod_paged_store(0, turned[0], turned[1], plan)
+    assert torch.equal(p.cache.pod_paged_prefill(0, None, None, turned[2], None, plan, p.scale), out)
+    p.expect(True)
