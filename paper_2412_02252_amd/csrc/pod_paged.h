@@ -47,8 +47,6 @@ struct pod_paged_plan_view {
 inline __host__ __device__ int pod_paged_tile_tokens(int rep) { return kPagedTileRows / rep; }
 pod_paged_plan_view pod_paged_plan_at(const void *plan, int rep, int n, int rows, size_t *bytes);
 
-typedef const __attribute__((address_space(1))) pod_u32x4 *pod_gvec;
-
 int pod_launch_paged_reset(const pod_paged *c, hipStream_t st);
 int pod_launch_paged_clear(const pod_paged *c, hipStream_t st); // the flag, and what refused extends left in room
 int pod_launch_paged_extend(const pod_paged *c, const int32_t *counts, const int32_t *slots, int n, hipStream_t st);

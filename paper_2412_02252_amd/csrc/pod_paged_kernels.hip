@@ -12,8 +12,6 @@ namespace {
 
 constexpr int kBook = 1024; // threads of a bookkeeping workgroup
 
-typedef __attribute__((ext_vector_type(4))) int i32x4;
-
 __device__ inline int lane_id() { return threadIdx.x & 63; }
 
 // Exclusive prefix sum over the workgroup and the total.  Called by all threads; what they wrote to memory and LDS before, all see after.
@@ -435,14 +433,15 @@ __global__ __launch_bounds__(kBook) void paged_plan_kernel(pod_paged_view c, con
         hi = cu[e + 1];
         bad = slot < 0 || slot >= c.B || lo < 0 || hi < lo || hi > rows || (e == 0 && lo != 0) || (e == n - 1 && hi != rows);
         if (!bad) {
-            len = c.lens[slot];
-            bad = mark(seen, slot) || len < hi - lo || len > c.maxctx || c.room[slot] < hi - lo;
+            const int held = c.lens[slot], room = c.room[slot]; // (both under way at once)
+            len = held;
+            bad = mark(seen, slot) || len < hi - lo || len > c.maxctx || room < hi - lo;
         }
         if (c.nw && !bad && hi > lo) {
             // What the rows attend by their own layers' keys starts at the first row's window (sink pages never go back).  Pages go back oldest
             // first, so the rest is there if that window's first page behind the sink is.
-            const int first = len - (hi - lo), page = max((c.S + c.ps - 1) / c.ps, max(first - c.W + 1, 0) / c.ps);
-            bad = (int64_t)page * c.ps < len && c.wtable[(size_t)slot * c.width + page] < 0;
+            const int shift = 31 - __clz(c.ps), first = len - (hi - lo), page = max((c.S + c.ps - 1) >> shift, max(first - c.W + 1, 0) >> shift);
+            bad = page <= (len - 1) >> shift && c.wtable[(size_t)slot * c.width + page] < 0;
         }
     }
     const bool refused = __syncthreads_or(bad) || n == 0;
