@@ -640,7 +640,8 @@ typedef struct pod_paged_config {
     pod_config base;          /* max_batch <= 1024 here */
     int32_t page_size;        /* tokens per page: 16, 32, 64, 128 or 256 */
     int32_t num_pages;        /* context pages */
-    int32_t num_window_pages; /* window pages; 0 if and only if no layer is an upper layer */
+    int32_t num_window_pages; /* window pages; 0 if and only if no layer is an upper layer.  An extend takes as many of them as context pages: a chunk's
+                                 tokens all need theirs until the next extend, beside every sequence's sinks and window */
     int32_t dtype;            /* POD_TYPE_*: keys, values, queries and outputs */
 } pod_paged_config;
 

@@ -10,7 +10,9 @@
 //    both, so a lane keeps one head's maximum and sum, and its probabilities are already the second product's operand.  K rows are loaded whole
 //    (one request = four rows of 256 bytes) and turned through a piece of LDS of the wave; V is turned in registers (v_perm_b32).
 //  - The new token's row is read from the call's arguments by the wave that has the last tile, and stored by it: no wait in between.
-// 16 sequences of 4096 .. 32768 tokens x 8 kv heads x 128 (1087 MB): 181 us, 6.0 TB/s; one of 32768 (134 MB): 33 us; 32 of 300 .. 4096 x 4 x 64 (47 MB): 17.6.
+// 16 sequences of 4096 .. 32768 tokens x 8 kv heads x 128 (1087 MB): 179 us, 6.1 TB/s; one of 32768 (134 MB): 33 us; 32 of 300 .. 4096 x 4 x 64 (47 MB): 17.8.
+// Weights are rounded to the type for the second product, whose operands have 16 bits (error against 64 bits 1.2 to 1.4 times that of rounding the result alone); the
+// sum that divides them, the maximum and all sums of products keep 32.
 // At an upper layer the list of a pair is its distant tiles (the lowest layer's keys and query), then the sink and window tiles (own keys,
 // window pages); a tile with both kinds is in both parts, each masking what is the other's.
 #include "pod_paged.h"

@@ -5,7 +5,7 @@
 // threads interleave: the lowest free page goes to the first (entry, token) that needs one.  What follows from it (rows and tables to
 // copy) is spread over the chip by a second launch that reads the decision from the cache's scratch memory.
 // Latency bounds the decisions (4 to 8 us each, a few dependent loads and prefix sums), the copy rate what follows: 64 forks of 8 prompts in 8 layers copy
-// 140 MB, read and written, in 22 us; compaction of 16 documents' cache after 8 ended moves 708 MB in 139 us (5.0 TB/s).
+// 140 MB, read and written, in 22 us; compaction of 16 documents' cache after 8 ended moves 708 MB in 137 to 139 us (5.1 TB/s).
 #include "pod_paged.h"
 
 namespace {
