@@ -2,7 +2,7 @@
 //
 // What bounds them is the matrix instructions, 4 D flops per (row, query head, key).  The tiles of all sequences are one list, longest first
 // (paged_plan_kernel), whose length the host bounds by the rows alone: workgroups past its end leave at once.  4 documents of 2000 .. 8192 tokens x
-// 32/8 heads x 128: 736 to 764 us from box to box, up to 1.0 PFLOP/s; 20 .. 700 tokens on 4096 .. 16384 held ones, 8 sequences: 419 to 432 us, up to 0.91
+// 32/8 heads x 128: 736 to 764 us from card to card, up to 1.0 PFLOP/s; 20 .. 700 tokens on 4096 .. 16384 held ones, 8 sequences: 419 to 432 us, up to 0.91
 // (these launches alone; the stores before them take 26 and 7).
 #include <mutex>
 
